@@ -450,7 +450,9 @@ int nova_causal_conv1d(const nova_sequences* sequences_host, int type, const nov
  * apart; channels / groups consecutive channels share a group.  `type` is theirs; A, D, delta_bias and the state
  * [slots, channels, states] are float.  1 <= states <= 64; groups divides channels.  D_dev, delta_bias_dev, state_dev and
  * z.data_dev may be null.  y overlaps no input.  One dense token for each sequence (tokens = 1: a serving step) takes a
- * kernel of its own.  The decays of up to eight tokens are multiplied with each other: below 2^-126 such a product is 0; where
+ * kernel of its own.  An A beyond 2^127 in magnitude, infinities included, counts as a number of that magnitude: a step dt of 0
+ * keeps the state and one from 2^-120 on leaves nothing of it (A < 0).
+ * The decays of up to eight tokens are multiplied with each other: below 2^-126 such a product is 0; where
  * growth (A > 0) takes it out of float's range, states and outputs are infinite or NaN.
  */
 typedef struct {

@@ -77,6 +77,7 @@ def selective_scan(u, delta, A, B, C, seqs, D=None, z=None, delta_bias=None, sof
     decay is off by (6 |dt A| + 4) u, a product and a sum 2u more; the input dt u B by 7u.  The bound takes 8 for each."""
     dtype, f = u.dtype, lambda a: a.double()
     ch = u.shape[1]
+    A = A.clamp(-torch.finfo(torch.float32).max, torch.finfo(torch.float32).max)         # as the header says of infinities
     at = torch.arange(ch, device=u.device) // (ch // B.shape[1])
     y = torch.full(u.shape, float("nan"), dtype=torch.float64, device=u.device)
     bound = torch.zeros_like(y)

@@ -35,6 +35,14 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) { return __
 __device__ __forceinline__ float2 mul2(float2 a, float2 b) { return __fmul2_rn(a, b); }
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
+// An infinite A (or A log2(e)) counts as float's number of that sign with the largest magnitude: the decay is 0 for any step from
+// 2^-120 on, and for a step of 0, which tokens behind the end have too, it is 1 and no NaN.
+__device__ __forceinline__ float finite(float A) {
+  asm("min.NaN.f32 %0, %0, 0f7F7FFFFF;" : "+f"(A));
+  asm("max.NaN.f32 %0, %0, 0fFF7FFFFF;" : "+f"(A));
+  return A;
+}
+
 // Four neighbouring values in one access
 __device__ __forceinline__ void load_quad(const float* p, float2 (&v)[2]) {
   const float4 w = *reinterpret_cast<const float4*>(p);
@@ -212,8 +220,8 @@ __global__ void __launch_bounds__(32 * kMaxWarps, RESIDENT) scan_kernel(const __
 #pragma unroll
   for (int j = 0; j < NS; ++j) {
     const int n = q * NS + j;
-    A[j].x = has0 && n < N ? a.A[(size_t)(d0 + ch) * N + n] * kLog2e : 0.f;
-    A[j].y = has1 && n < N ? a.A[(size_t)(d0 + ch + 1) * N + n] * kLog2e : 0.f;
+    A[j].x = has0 && n < N ? finite(a.A[(size_t)(d0 + ch) * N + n] * kLog2e) : 0.f;
+    A[j].y = has1 && n < N ? finite(a.A[(size_t)(d0 + ch + 1) * N + n] * kLog2e) : 0.f;
   }
   const float2 bias = make_float2(a.bias && has0 ? a.bias[d0 + ch] : 0.f, a.bias && has1 ? a.bias[d0 + ch + 1] : 0.f);
   const float2 skip = make_float2(a.D && has0 ? a.D[d0 + ch] : 0.f, a.D && has1 ? a.D[d0 + ch + 1] : 0.f);
@@ -422,7 +430,7 @@ __global__ void __launch_bounds__(kStepThreads, 4) step_kernel(const __grid_cons
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if (!WHOLE && j >= here) continue;                     // an infinite dt u times a zero behind the last state
-        h[r][j] = fmaf(ex2(dtr * Ar[r][j]), h[r][j], dur * B[j]);
+        h[r][j] = fmaf(ex2(dtr * finite(Ar[r][j])), h[r][j], dur * B[j]);
         if (WHOLE && here == 0) continue;
         y[r] = fmaf(C[j], h[r][j], y[r]);
       }
