@@ -73,6 +73,9 @@ __device__ __forceinline__ void load_states(const T* p, float (&v)[NS]) {
   }
 }
 
+// A behind the last state: not 0, so that its product with an infinite step is no NaN that a C of 0 would pass on to y
+constexpr float kNoState = -1.17549435e-38f;
+
 constexpr int TC = 8;            // tokens of a piece: one for each of the eight lanes that share two channels
 // What a warp keeps in shared memory.  NS states a lane, 8 NS >= states.
 template <typename T, int NS>
@@ -220,8 +223,8 @@ __global__ void __launch_bounds__(32 * kMaxWarps, RESIDENT) scan_kernel(const __
 #pragma unroll
   for (int j = 0; j < NS; ++j) {
     const int n = q * NS + j;
-    A[j].x = has0 && n < N ? finite(a.A[(size_t)(d0 + ch) * N + n] * kLog2e) : 0.f;
-    A[j].y = has1 && n < N ? finite(a.A[(size_t)(d0 + ch + 1) * N + n] * kLog2e) : 0.f;
+    A[j].x = has0 && n < N ? finite(a.A[(size_t)(d0 + ch) * N + n] * kLog2e) : kNoState;
+    A[j].y = has1 && n < N ? finite(a.A[(size_t)(d0 + ch + 1) * N + n] * kLog2e) : kNoState;
   }
   const float2 bias = make_float2(a.bias && has0 ? a.bias[d0 + ch] : 0.f, a.bias && has1 ? a.bias[d0 + ch + 1] : 0.f);
   const float2 skip = make_float2(a.D && has0 ? a.D[d0 + ch] : 0.f, a.D && has1 ? a.D[d0 + ch + 1] : 0.f);
