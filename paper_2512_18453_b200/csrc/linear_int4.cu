@@ -387,10 +387,23 @@ int start(Int4Args a, cudaStream_t s) {
     if (int e = start<T, LOG_GROUP>(a, s)) return e;
     return start<T, LOG_GROUP>(b, s);
   }
+  const int row_blocks = (tiles + a.tiles - 1) / a.tiles;
+  if (row_blocks > 65535) {                      // as many as a grid may have in this direction: half of the outputs at a time
+    Int4Args b = a;
+    a.N = tiles / 2 * 16;
+    b.N -= a.N;
+    b.codes += (size_t)a.N * (a.K / 2);
+    b.scales = (const T*)b.scales + (size_t)a.N * (a.K >> LOG_GROUP);
+    if (b.zeros) b.zeros += (size_t)a.N * (a.K >> LOG_GROUP);
+    if (b.bias) b.bias = (const T*)b.bias + a.N;
+    b.y = (T*)b.y + a.N;
+    if (int e = start<T, LOG_GROUP>(a, s)) return e;
+    return start<T, LOG_GROUP>(b, s);
+  }
   auto kernel = linear_kernel<T, TILES, LOG_GROUP>;
   if (int e = (int)allow_dynamic_smem<kMostSmem>(kernel)) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(split, (tiles + a.tiles - 1) / a.tiles);
+  cfg.gridDim = dim3(split, row_blocks);
   cfg.blockDim = dim3(32 * warps);
   cfg.dynamicSmemBytes = at.bytes;
   cfg.stream = s;
