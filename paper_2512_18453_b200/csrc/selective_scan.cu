@@ -465,7 +465,6 @@ template <typename T, int R, bool WHOLE>
 int start_step(const ScanArgs& a, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)a.q.count, (a.channels + kStepWidth * R - 1) / (kStepWidth * R));
-  if (cfg.gridDim.y > 65535) return (int)cudaErrorInvalidConfiguration;
   cfg.blockDim = dim3(kStepThreads);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
@@ -486,7 +485,8 @@ int start_step(const ScanArgs& a, cudaStream_t s) {
 
 template <typename T>
 int start(const ScanArgs& a, cudaStream_t s) {
-  if (!a.q.cu && a.q.tokens == 1) return start_step<T>(a, s);
+  // the blocks of channels are the step kernel's second grid dimension
+  if (!a.q.cu && a.q.tokens == 1 && a.channels <= 65535 * kStepWidth) return start_step<T>(a, s);
   return a.states <= 16 ? start_pieces<T, 2>(a, s) : a.states <= 32 ? start_pieces<T, 4>(a, s) : start_pieces<T, 8>(a, s);
 }
 
