@@ -433,10 +433,12 @@ typedef struct {
 
 /*
  * Causal convolution per channel: y[t, d] = act(bias[d] + sum_{k < width} weight[d, k] * x[t - width + 1 + k, d]), where the
- * inputs before a sequence's first token are its state's (zeros without one).  weight_dev [channels, width], 2 <= width <= 4;
+ * inputs before a sequence's first token are its state's (zeros without one).  channels <= NOVA_CONV1D_MAX_CHANNELS;
+ * weight_dev [channels, width], 2 <= width <= 4;
  * bias_dev [channels] or null; state_dev [slots, width - 1, channels], oldest first, or null; all of the same type as x and y,
  * summed in float, the state an exact copy of inputs.  y overlaps no input.  flags: NOVA_SILU.
  */
+#define NOVA_CONV1D_MAX_CHANNELS (65535 * 256)
 int nova_causal_conv1d(const nova_sequences* sequences_host, int type, const nova_rows* x_host, const void* weight_dev,
                        const void* bias_dev, int channels, int width, void* state_dev, const nova_rows* y_host, int flags,
                        nova_stream stream);

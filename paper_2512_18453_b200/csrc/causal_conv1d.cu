@@ -217,14 +217,14 @@ int start(ConvArgs a, cudaStream_t s) {
   while (across > 32 && (columns + across - 1) / across * across > (columns + 31) / 32 * 32 * 11 / 10) across /= 2;
   while (across / 2 >= columns) across /= 2;
   const int down = kThreads / across;
-  const int column_blocks = (columns + across - 1) / across;
+  const int column_blocks = (columns + across - 1) / across;           // 65535 at most: kThreads across and two channels each
   // one wave of CTAs where there are rows enough, so that each streams until the end
   const long long rows = a.q.cu ? a.q.tokens : a.q.tokens * a.q.count, wave = 148ll * resident(WHOLE) * down / column_blocks;
   long long run = (rows + wave) / (wave + 1);
   run = (run + AHEAD - 1) / AHEAD * AHEAD;
   a.run = (int)(run < AHEAD ? AHEAD : run > 4096 ? 4096 : run);
   const long long runs = (a.q.tokens + a.run - 1) / a.run, items = a.q.cu ? a.q.count + runs : a.q.count * runs;
-  if (items >= INT32_MAX || column_blocks > 65535) return (int)cudaErrorInvalidConfiguration;
+  if (items >= INT32_MAX) return (int)cudaErrorInvalidConfiguration;
   a.items = (unsigned)items;
   a.runs = (unsigned)runs;
   a.runs_shift = 0;
@@ -263,7 +263,7 @@ extern "C" int nova_causal_conv1d(const nova_sequences* q, int type, const nova_
                                   int channels, int width, void* state, const nova_rows* y, int flags, nova_stream stream) {
   using namespace nova;
   using namespace nova::mix;
-  if (!type_ok(type) || !seqs_ok(q, state != nullptr) || !x || !y || channels <= 0 || width < 2 || width > 4 || (flags & ~NOVA_SILU))
+  if (!type_ok(type) || !seqs_ok(q, state != nullptr) || !x || !y || channels <= 0 || channels > NOVA_CONV1D_MAX_CHANNELS || width < 2 || width > 4 || (flags & ~NOVA_SILU))
     return NOVA_ERR_INVALID_ARG;
   if (q->sequences == 0 || q->tokens == 0) return NOVA_OK;
   const size_t e = type_bytes(type);

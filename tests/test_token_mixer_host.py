@@ -145,3 +145,13 @@ def test_oracle_int4_unpacks_low_bits_first():
 def test_oracle_sequences_follow_the_header():
     assert ref.sequences(3, 10, [-4, 3, 3, 20], [2, 0, 9], [True, False, True], 4) == [(0, 0, 3, 2, True)]
     assert ref.sequences(2, 5) == [(0, 0, 5, None, False), (1, 5, 10, None, False)]
+
+
+def test_conv_refuses_more_channels_than_the_header_allows():
+    most = 65535 * 256
+    text = open(os.path.join(os.path.dirname(__file__), "..", "include", "nova.h")).read()
+    assert re.search(r"NOVA_CONV1D_MAX_CHANNELS \((.*)\)", text).group(1) == "65535 * 256"
+    wide = dict(x=(P, most + 1, 4 * most), y=(P + 4096, most + 1, 4 * most))
+    assert conv(D=most + 1, **wide) == INVALID and conv(seqs(B=0), D=most, **wide) == 0
+    if not torch.cuda.is_available():
+        assert conv(D=most, **wide) == CUDA
