@@ -473,9 +473,9 @@ int nova_selective_scan(const nova_sequences* sequences_host, int type, const no
  * codes_dev [N, K / 2] bytes, the code of an even k in the low four bits; scales_dev [N, K / group] of the type of x and y
  * (NOVA_F16 or NOVA_BF16); zeros_dev [N, K / group] bytes (0 .. 15, larger ones modulo 16), or null: 8 everywhere; bias_dev [N]
  * or null.  group is 32, 64 or 128 and divides K; 1 <= M <= NOVA_INT4_MAX_ROWS, N <= NOVA_INT4_MAX_N, K <= NOVA_INT4_MAX_K.
- * x_row, y_row: elements between rows.  No weight is rounded: codes and zeros are taken exactly, a group's sum is
- * sum(x q) - zero * sum(x), each summed in float, and is multiplied by its scale in float.  An infinite or NaN x makes all
- * outputs of its row infinite or NaN.  codes_dev is 16-byte aligned; y overlaps no input.
+ * x_row, y_row: elements between rows.  No weight is rounded: codes less zeros are taken exactly, a group's sum of x (q - z) is
+ * float, and so is its product with the scale.  An infinite or NaN x makes all outputs of its row infinite or NaN.  codes_dev is
+ * 16-byte aligned; y overlaps no input.
  */
 #define NOVA_INT4_MAX_ROWS 16
 #define NOVA_INT4_MAX_N (1 << 26)

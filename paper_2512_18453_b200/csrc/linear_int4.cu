@@ -5,10 +5,9 @@
 // group is multiplied by the group's scale in float, so that no weight is rounded.  The order of k is free in such a sum: the four
 // lanes of a row take neighbouring words, eight codes each, and the elements of x that go with them.
 //
-// What bounds it: not the bytes but the way from codes to products (five to eight integer instructions for eight codes, at half the
-// issue rate), x from shared memory, and what a CTA does before its first product.  1 x 4096 x 4096 half 6.4 us (floor 1.4),
-// 1 x 14336 x 8192 half 20 (9.5), 16 x 14336 x 8192 bf16 in groups of 64 41 us (10): 3.0 and 1.6 TB/s; the schedulers issue in 43 % of
-// the cycles there, the tensor pipe is busy for 18 %.
+// What bounds it: not the bytes but the way from codes to products (five to seven integer instructions for eight codes, at half the
+// issue rate, and four to take off the zero), x from shared memory, and what a CTA does before its first product.  1 x 4096 x 4096
+// half 6.4 us (floor 1.4), 1 x 14336 x 8192 half 20.9 (9.5), 16 x 14336 x 8192 bf16 in groups of 64 35.5 us (10): 2.9 and 1.8 TB/s.
 #include <cooperative_groups.h>
 
 #include <type_traits>
@@ -48,30 +47,33 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(z0), "f"(z1), "f"(z2), "f"(z3));
 }
 
-// The eight codes of a word as numbers of the type; pair p holds codes p and p + 4.
-// half: the bits of a code, as they are, are a subnormal number, q 2^-24, and those of its neighbour, four bits up, 16 q 2^-24; pairs 0
-// and 2 come as the first, 1 and 3 as the second, and have a sum each.  bfloat16, whose subnormals are beyond float's range once
-// multiplied: the code as the upper bits of the mantissa of 1, 1 + q / 16.  All exact.  That is what the zero is subtracted from after
-// the sum, as (zero + OFFSET) times the sum of x: sums of x q and not of x (q - zero), whose roundings are larger by the ratio
-// of (q + OFFSET) to |q - zero|, some six, and are still float's.
+// The eight codes of a word, less their zero, as numbers of the type; pair p holds codes p and p + 4.  All exact, so that a code
+// equal to its zero adds nothing.
+// half: the bits of a code, as they are, are a subnormal number, q 2^-24, and those of its neighbour, four bits up, 16 q 2^-24,
+// which a multiply-add takes to the first's unit.  bfloat16, whose subnormals are beyond float's range once multiplied: the bits are
+// the lowest of the mantissa of 128, 128 + q, and 128 + zero is taken off.
 template <typename T> struct Codes;
 template <> struct Codes<__half> {
-  static constexpr float OFFSET = 0.f, RATIO = 16.f, UNIT = 1048576.f;      // codes = UNIT (RATIO * (pairs 0, 2) + (pairs 1, 3)) - OFFSET
-  __device__ __forceinline__ static void numbers(uint32_t w, uint32_t (&out)[4]) {
-    out[0] = w & 0x000f000fu;
-    out[1] = w & 0x00f000f0u;
-    out[2] = (w >> 8) & 0x000f000fu;
-    out[3] = (w >> 8) & 0x00f000f0u;
+  static constexpr uint32_t BASE = 0;
+  static constexpr float UNIT = 16777216.f;                     // codes in units of the numbers
+  using Pair = __half2;
+  __device__ __forceinline__ static Pair pair(uint32_t bits) { return *reinterpret_cast<const Pair*>(&bits); }
+  __device__ __forceinline__ static void numbers(uint32_t w, uint32_t, Pair zero, Pair (&out)[4]) {
+    const Pair sixteenth = __float2half2_rn(1.f / 16), less = __hneg2(zero);
+    out[0] = __hsub2(pair(w & 0x000f000fu), zero);
+    out[1] = __hfma2(pair(w & 0x00f000f0u), sixteenth, less);
+    out[2] = __hsub2(pair((w >> 8) & 0x000f000fu), zero);
+    out[3] = __hfma2(pair((w >> 8) & 0x00f000f0u), sixteenth, less);
   }
 };
 template <> struct Codes<__nv_bfloat16> {
-  static constexpr float OFFSET = 16.f, RATIO = 1.f, UNIT = 16.f;
-  static constexpr uint32_t ONE = 0x3f803f80u;
-  __device__ __forceinline__ static void numbers(uint32_t w, uint32_t (&out)[4]) {
-    out[0] = ((w << 3) & 0x00780078u) | ONE;
-    out[1] = ((w >> 1) & 0x00780078u) | ONE;
-    out[2] = ((w >> 5) & 0x00780078u) | ONE;
-    out[3] = ((w >> 9) & 0x00780078u) | ONE;
+  static constexpr uint32_t BASE = 0x43004300u;
+  static constexpr float UNIT = 1.f;
+  using Pair = __nv_bfloat162;
+  __device__ __forceinline__ static Pair pair(uint32_t bits) { return *reinterpret_cast<const Pair*>(&bits); }
+  __device__ __forceinline__ static void numbers(uint32_t w, uint32_t base, Pair zero, Pair (&out)[4]) {
+#pragma unroll
+    for (int p = 0; p < 4; ++p) out[p] = __hsub2(pair(((w >> 4 * p) & 0x000f000fu) | base), zero);
   }
 };
 
@@ -79,14 +81,13 @@ constexpr int kChunk = 128;                       // k of a warp's step: four wo
 constexpr int kMaxSplit = 8;                      // CTAs of a cluster, which share k
 constexpr int kMostSmem = 227 * 1024;
 
-// Shared memory: x of the CTA's k as the operand wants it, rows 64 bytes apart modulo the 128 of the banks; the sums of x over each
-// group; for each warp scale and scaled zero of its 16 outputs and groups, rows two banks apart; the sums of the products.
+// Shared memory: x of the CTA's k as the operand wants it, rows 64 bytes apart modulo the 128 of the banks; for each warp scale and
+// zero of its 16 outputs and groups, rows two banks apart; the sums of the products.
 struct Layout {
-  int x_row, sums, table, table_row, part, bytes;             // in bytes
+  int x_row, table, table_row, part, bytes;             // in bytes
   __host__ __device__ Layout(int warps, int M, int k_range, int k_part, int part_floats, int log_group) {
     x_row = (2 * k_range + 127) / 128 * 128 + 64;
-    sums = M * x_row;
-    table = sums + 16 * (k_range >> log_group) * 4;
+    table = M * x_row;
     table_row = (((k_part >> log_group) + 15) / 16 * 16 + 1) * 8;
     part = table + warps * 16 * table_row;
     bytes = part + part_floats * 4;
@@ -95,7 +96,8 @@ struct Layout {
 
 // The sums run over the four lanes of a row, so that every group has to be spread over all four.  Of a group of 128 a lane's share is
 // 16 bytes, of one of 64 it is 8.  Of one of 32 it would be 4: there a lane loads 16 bytes too, a whole group, and the four lanes
-// transpose their words (1 x 14336 x 8192: 30.7 us, 36.8 with loads of 4; the same for groups of 64, 16 rows, is 41.8 against 40.6).
+// transpose their words (1 x 14336 x 8192 when the zero was taken off after the sum: 30.7 us, 36.8 with loads of 4; the same for groups
+// of 64, 16 rows, 41.8 against 40.6).
 __device__ __forceinline__ void transpose(uint32_t (&w)[4], int q) {
   auto swap = [](bool upper, uint32_t& low, uint32_t& high, int m) {           // the lower lane's high with the upper lane's low
     const uint32_t got = __shfl_xor_sync(0xffffffffu, upper ? low : high, m);
@@ -158,6 +160,9 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) linear_kernel(const __grid_
       aim();
     }
   };
+  // BASE, but not as a constant: an instruction takes one, and the mask of the codes is one already (M > 0; 1 x 14336 x 8192 bfloat16
+  // 21.9 us, 25.9 with two)
+  const uint32_t base = Codes<T>::BASE | (uint32_t)(a.M >> 31);
   uint32_t held[DEPTH][2][4];
   if (steps > 0) {
     aim();
@@ -166,10 +171,8 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) linear_kernel(const __grid_
   }
 
   // x as pairs (0, 4), (1, 5), (2, 6), (3, 7) of eight elements, in the order of the products: pairs 0 and 2, then 1 and 3.  Piece
-  // WORDS q + i of a group goes with word i of lane q and stands where the four lanes of word i find theirs side by side.  The lanes
-  // of a group add it up.
+  // WORDS q + i of a group goes with word i of lane q and stands where the four lanes of word i find theirs side by side.
   constexpr int PIECES = 1 << (LOG_GROUP - 3), BATCH = 4;
-  float* sums = reinterpret_cast<float*>(smem + at.sums);
   const int per_row = (k_count + kChunk - 1) / kChunk * (kChunk / 8);          // a multiple of 16: no group is cut
   for (int i0 = warp * 32; i0 < a.M * per_row; i0 += BATCH * blockDim.x) {
     uint32_t v[BATCH][4];
@@ -193,20 +196,11 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) linear_kernel(const __grid_
     for (int j = 0; j < BATCH; ++j) {
       if (i0 + j * (int)blockDim.x >= a.M * per_row) break;
       const int i = i0 + j * blockDim.x + lane, m = i / per_row, piece = i - m * per_row;
-      float s = 0.f;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float2 f = load_pair(reinterpret_cast<const T*>(&v[j][e]));
-        s += f.x + f.y;
-      }
-#pragma unroll
-      for (int o = PIECES / 2; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
       if (m >= a.M) continue;
       const int in_group = piece % PIECES, place = piece - in_group + in_group % WORDS * 4 + in_group / WORDS;
       *reinterpret_cast<uint4*>(smem + m * at.x_row + 16 * place) =
           make_uint4(__byte_perm(v[j][0], v[j][2], 0x5410), __byte_perm(v[j][1], v[j][3], 0x5410), __byte_perm(v[j][0], v[j][2], 0x7632),
                      __byte_perm(v[j][1], v[j][3], 0x7632));
-      if (in_group == 0 && 8 * piece < k_count) sums[(8 * piece >> LOG_GROUP) * 16 + m] = s;
     }
   }
   __syncthreads();
@@ -216,13 +210,13 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) linear_kernel(const __grid_
   const int table_row = at.table_row / 8, groups = my_count >> LOG_GROUP, all_groups = a.K >> LOG_GROUP;
   const T* scales = (const T*)a.scales + ((k_first + my_k) >> LOG_GROUP);
   const unsigned char* zeros = a.zeros + ((k_first + my_k) >> LOG_GROUP);
-  auto entry = [](float scale, int zero) { return make_float2(scale * Codes<T>::UNIT, -scale * ((float)zero + Codes<T>::OFFSET)); };
+  auto entry = [](float scale, uint32_t zero) { return make_float2(scale * Codes<T>::UNIT, __uint_as_float(Codes<T>::BASE | zero * 0x10001u)); };
   const unsigned char* x_of_lane[TILES];
 #pragma unroll
   for (int t = 0; t < TILES; ++t)              // rows of x behind the last are read as that one: what comes of them is not stored
     x_of_lane[t] = smem + min(8 * t + g, a.M - 1) * at.x_row + 2 * my_k + 16 * q;
   for (int tile = warp / a.wk; tile < t_count; tile += stride) {
-    // scale and -scale * (zero + OFFSET) (exact: 11 bits by 5) as float, what the sums are multiplied by
+    // the scale as float, what the sums are multiplied by, and the zero as it is taken off a pair of codes
     __syncwarp();
     if (a.table_vec) {                                        // eight groups at once
       const int per_row = groups >> 3;
@@ -246,7 +240,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) linear_kernel(const __grid_
       for (int i = lane; i < 16 * groups; i += 32) {
         const int r = i / groups, h = i - r * groups;
         const size_t n = (size_t)min((t_first + tile) * 16 + r, a.N - 1) * all_groups + h;
-        table[r * table_row + h] = entry(to_float(scales[n]), a.zeros ? zeros[n] & 15 : 8);
+        table[r * table_row + h] = entry(to_float(scales[n]), a.zeros ? zeros[n] & 15u : 8u);
       }
     }
     __syncwarp();
@@ -254,10 +248,10 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) linear_kernel(const __grid_
 #pragma unroll
     for (int i = 0; i < TILES * 4; ++i) (&sum[0][0])[i] = 0.f;
     const float2* my_table = table + g * table_row;
-    const float* my_sums = sums + (my_k >> LOG_GROUP) * 16 + 2 * q;
     const unsigned char* xs[TILES];
 #pragma unroll
     for (int t = 0; t < TILES; ++t) xs[t] = x_of_lane[t];
+    auto bits = [](const auto& pair) { return *reinterpret_cast<const uint32_t*>(&pair); };
     auto products = [&](const uint32_t (&held)[2][4], int step) {
       uint32_t words[2][4];
 #pragma unroll
@@ -270,38 +264,30 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) linear_kernel(const __grid_
 #pragma unroll
       for (int h = 0; h < HELD; ++h) {
         if (h >= left) break;
-        float c[TILES][2][4];                                   // sums of pairs 0 and 2, of 1 and 3
+        const float2 entry0 = my_table[h], entry1 = my_table[8 * table_row + h];
+        const auto zero0 = Codes<T>::pair(__float_as_uint(entry0.y)), zero1 = Codes<T>::pair(__float_as_uint(entry1.y));
+        float c[TILES][4];
 #pragma unroll
         for (int u = 0; u < WORDS; ++u) {
-          uint32_t r0[4], r1[4];
-          Codes<T>::numbers(words[0][h * WORDS + u], r0);
-          Codes<T>::numbers(words[1][h * WORDS + u], r1);
-          const uint32_t f0[4] = {r0[0], r1[0], r0[2], r1[2]}, f1[4] = {r0[1], r1[1], r0[3], r1[3]};
+          typename Codes<T>::Pair r0[4], r1[4];
+          Codes<T>::numbers(words[0][h * WORDS + u], base, zero0, r0);
+          Codes<T>::numbers(words[1][h * WORDS + u], base, zero1, r1);
+          const uint32_t f0[4] = {bits(r0[0]), bits(r1[0]), bits(r0[2]), bits(r1[2])}, f1[4] = {bits(r0[1]), bits(r1[1]), bits(r0[3]), bits(r1[3])};
 #pragma unroll
           for (int t = 0; t < TILES; ++t) {
             const uint4 x = *reinterpret_cast<const uint4*>(xs[t] + 64 * (h * WORDS + u));
-            mma<T>(c[t][0], f0, x.x, x.y, u == 0);
-            mma<T>(c[t][1], f1, x.z, x.w, u == 0);
+            mma<T>(c[t], f0, x.x, x.y, u == 0);
+            mma<T>(c[t], f1, x.z, x.w, false);
           }
         }
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const float2 scale = my_table[8 * r * table_row + h];
+        for (int t = 0; t < TILES; ++t)
 #pragma unroll
-          for (int t = 0; t < TILES; ++t) {
-            const float2 of_x = *reinterpret_cast<const float2*>(my_sums + h * 16 + 8 * t);
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              float& s = sum[t][2 * r + e];
-              s = fmaf(scale.x, fmaf(c[t][0][2 * r + e], Codes<T>::RATIO, c[t][1][2 * r + e]), fmaf(scale.y, e ? of_x.y : of_x.x, s));
-            }
-          }
-        }
+          for (int e = 0; e < 4; ++e) sum[t][e] = fmaf(e < 2 ? entry0.x : entry1.x, c[t][e], sum[t][e]);
       }
 #pragma unroll
       for (int t = 0; t < TILES; ++t) xs[t] += 2 * kChunk;
       my_table += HELD;
-      my_sums += HELD * 16;
     };
     // DEPTH steps at a time; the steps of a tile are a multiple of that but for its last turn, after which what is held moves up
     for (int step = 0; step < steps; step += DEPTH) {
