@@ -269,7 +269,14 @@ static PyObject* output(PyObject* out, PyObject* x, const long long* n, int lead
     if (!out) return NULL;
   }
   int ok = tensor(out, dtype, dev, 0, t) && t->dims == lead + 1 && t->size[lead] == cols;
-  for (int i = 0; ok && i < lead; ++i) ok = t->size[i] == n[i] && (n[i] <= 1 || t->stride[i] >= cols);
+  for (int i = 0; ok && i < lead; ++i) ok = t->size[i] == n[i];
+  const int near = lead == 2 && (n[0] <= 1 || (n[1] > 1 && t->stride[1] <= t->stride[0]));      /* the dimension of the smaller stride */
+  long long wide = cols;                                                                        /* of what the other one repeats */
+  for (int k = 0, i = near; ok && k < lead; ++k, i = !near)
+    if (n[i] > 1) {
+      ok = t->stride[i] >= wide;
+      wide += (n[i] - 1) * t->stride[i];
+    }
   if (!ok) Py_CLEAR(out);
   return out;
 }

@@ -103,9 +103,12 @@ def _token_rows(t, name, dtype, lead, inner):
 def _output(out, x, lead, D):
     if out is None:
         return _torch.empty((*lead, D), dtype=x.dtype, device=x.device)
-    for k in range(len(lead) - 1, -1, -1):             # rows that lie over each other would be written twice
-        if out.dim() == len(lead) + 1 and out.shape[k] > 1 and out.stride(k) < D:
-            raise ValueError("out: its rows overlap")
+    if out.dim() == len(lead) + 1:                     # rows that lie over each other would be written twice
+        wide = D                                       # of what is repeated with the next larger stride
+        for stride, n in sorted((out.stride(k), out.shape[k]) for k in range(len(lead)) if out.shape[k] > 1):
+            if stride < wide:
+                raise ValueError("out: its rows overlap")
+            wide += (n - 1) * stride
     return out
 
 

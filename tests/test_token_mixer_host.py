@@ -155,3 +155,16 @@ def test_conv_refuses_more_channels_than_the_header_allows():
     assert conv(D=most + 1, **wide) == INVALID and conv(seqs(B=0), D=most, **wide) == 0
     if not torch.cuda.is_available():
         assert conv(D=most, **wide) == CUDA
+
+
+def test_binding_tells_outputs_whose_rows_overlap():
+    x, buf = torch.zeros(2, 5, 32, dtype=torch.float16), torch.zeros(4096, dtype=torch.float16)
+    out = lambda strides, lead=(2, 5): tm._output(buf.as_strided((*lead, 32), (*strides, 1)), x, lead, 32)
+    for strides in ((32, 32), (0, 32), (32, 0), (31, 500), (500, 31), (64, 32), (159, 32), (33, 64), (40, 71), (128, 32)):
+        with pytest.raises(ValueError):
+            out(strides)
+    for strides in ((160, 32), (32, 64), (500, 40), (40, 72), (192, 40)):
+        assert out(strides).stride()[:2] == strides
+    assert out((0, 32), (1, 5)).shape == (1, 5, 32) and out((32, 0), (2, 1)).shape == (2, 1, 32) and out((32,), (5,)).shape == (5, 32)
+    with pytest.raises(ValueError):
+        out((31,), (5,))
