@@ -400,7 +400,8 @@ int nova_maxpool2x2(const void* x_dev, void* y_dev, int N, int H, int W, int C,
  * serving models whose layers run a short causal convolution and a selective state-space recurrence over tokens, and the
  * product of a few token rows with 4-bit weights.  Inference only, like every operator here.  Channels are innermost, as
  * in NHWC.  No plan: all pointers belong to the device that is current at the call.  Nothing is allocated, nothing
- * synchronises, and nothing is kept from call to call.  Sums and states are float; outputs are rounded once.
+ * synchronises, and nothing is kept from call to call.  Sums and states are float; outputs are rounded once.  v * sigmoid(v) is
+ * evaluated on v / 256: floats below 2^-118 in magnitude (weights, sums, gates) keep fewer bits there.
  */
 enum { NOVA_F32 = 0, NOVA_F16 = 1, NOVA_BF16 = 2 };   /* element types */
 enum { NOVA_SILU = 1,            /* causal convolution: y = v * sigmoid(v) */

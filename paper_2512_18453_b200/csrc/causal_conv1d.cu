@@ -2,9 +2,9 @@
 //
 // What bounds it: x read and y written once, 2 e bytes an element, and next to that the two special-function instructions of each
 // SiLU.  A thread slides a window of W inputs over a run of rows, 16 bytes each, with the next seven or eight in flight.
-// 2 x 4096 x 4096, 4 taps, bf16: 29.2 us (71 % of the copy rate), without SiLU 23.3 (89 %); 4096 x 4096 float without it 20.5
-// (101 %).  Where rows are on no such boundary, two channels a thread by themselves: 6000 packed rows of 777 halves 12.3 us (24 %),
-// bound by instructions.
+// 2 x 4096 x 4096, 4 taps, bf16: 29.2 us (71 % of the copy rate), without SiLU 23.3 (89 %); 4096 x 4096 float without it 20.7
+// (100 %), with it 22.5.  Where rows are on no such boundary, two channels a thread by themselves: 6000 packed rows of 777 halves
+// 12.3 us (24 %), bound by instructions; with 64 registers, for eight CTAs an SM, most of these spill 4 to 52 bytes.
 #include <type_traits>
 
 #include "sm100.cuh"
@@ -25,7 +25,7 @@ struct ConvArgs {
   const void *weight, *bias;
   void* state;
   int channels, silu;
-  int run;                         // rows of a run, a multiple of those in flight
+  int run;                         // rows of a run, at least those in flight
   unsigned items, runs;            // runs of rows: in all, and of a dense sequence or of all packed rows
   unsigned runs_mul, runs_shift;   // n / runs = (mulhi(n, mul) + n) >> shift for n < 2^31
 };
@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(kThreads, resident(WHOLE)) conv_kernel(const _
           for (int k = 0; k < W - 1; ++k) (k + len < W - 1 ? in[k + len] : next[k + len - (W - 1)]).store(state + (size_t)k * a.channels, second);
     }
   }
-  // weights and bias as float, with SiLU scaled by 1/256 (exactly) as silu_of_256th wants the sum
+  // weights and bias as float, with SiLU scaled by 1/256 as silu_of_256th wants the sum (exactly but for floats below 2^-118)
   float2 w[W][H], b[H], win[W - 1][H];
   const float scale = a.silu ? 1.f / 256 : 1.f;
   {
@@ -246,9 +246,12 @@ int start(const ConvArgs& a, cudaStream_t s) {
   constexpr int VEC = 16 / sizeof(T);
   const size_t e = sizeof(T);
   const bool vec = a.channels % VEC == 0 && rows_aligned(a.x, e, VEC * e) && rows_aligned(a.y, e, VEC * e) && aligned(a.state, VEC * e) && aligned(a.weight, VEC * e) && aligned(a.bias, VEC * e);
-  // Rows in flight: eight, seven where eight would spill (bf16 / half, 2 x 4096 x 4096: 8 rows 28.7 / 37.2 us, 7 rows 29.4 / 29.3).
+  // Rows in flight: eight, seven of two bytes with four taps, where eight do not fit the registers in half (bf16 / half, 2 x 4096 x
+  // 4096: 8 rows 28.7 / 37.2 us, 7 rows 29.2 / 29.3; of seven, half spills one register).
   constexpr int AHEAD = sizeof(T) == 2 && W == 4 ? 7 : 8;
-  if (vec && !a.q.cu && a.q.tokens <= 4) return start<T, W, 4, true, 4>(a, s);     // narrower, so that a token has more threads
+  // Short sequences: narrower, so that a token has more threads (channels a thread 8 / 4: one token of 1 x 1024 bf16 4.0 / 2.85 us, of
+  // 256 x 4096 12.1 / 11.8; four tokens of 64 x 4096 5.0 / 4.4; 64 tokens of it 23.2 / 25.9)
+  if (vec && !a.q.cu && a.q.tokens <= 4) return start<T, W, 4, true, 4>(a, s);
   return vec ? start<T, W, VEC, true, AHEAD>(a, s) : start<T, W, 2, false, 8>(a, s);
 }
 template <typename T>

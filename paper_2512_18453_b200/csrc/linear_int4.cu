@@ -22,7 +22,8 @@ using namespace mix;
 
 constexpr int kMaxWarps = 8;
 // CTAs at once: two on an SM, less what clusters of eight leave over.  One wave of them, each with as many tiles as it takes: several
-// waves of one tile each took 60 us where this takes 41.
+// waves of one tile each took 60 us where this took 41.  With many rows of a long k a CTA's shared memory passes half of an SM's (16 rows
+// of k = 11008 in groups of 32, 14336 outputs: 122 KB): one CTA an SM, and two waves.
 constexpr int kCtas = 264;
 
 struct Int4Args {

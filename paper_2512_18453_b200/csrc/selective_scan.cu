@@ -7,9 +7,11 @@
 // so that each exponential is computed once and all that passes from piece to piece is h.  Eight lanes share two channels, the
 // operands of the packed float instructions, and have NS states each.
 //
-// What bounds it: instructions.  1 x 4096 x 4096 with 16 states takes 192 us, 60 of which the exponentials would take by themselves
-// (16 a cycle and SM) and 21 the bytes; the schedulers issue in 65 % of the cycles, 8 instructions for each pair of exponentials
-// and as many again for the sums over lanes, step sizes, gates and copies; 512 CTAs of 296 resident at a time end unevenly.
+// What bounds it: instructions.  1 x 4096 x 4096 with 16 states takes 193 us; the special-function unit, 16 a cycle and SM, would take
+// 72 (58 for the exponentials of the decays, 14 for softplus and gate) and the bytes 21.  The schedulers issue in 65 % of the cycles,
+// 30 instructions of a warp for each pair of exponentials: nine are the recurrence and what the state before the piece adds, the
+// others make B and C float for each pair of channels, sum over lanes, and do step sizes, gates and copies.  512 CTAs, of which 296
+// are resident at a time, end unevenly.
 #include "sm100.cuh"
 #include "tma_host.h"
 #include "token_mixer.cuh"
@@ -126,7 +128,7 @@ struct Elements {
 };
 
 // EXACT: 8 NS states, none to mask.  QUICK: those, of two bytes, and everything on boundaries of 16 bytes; a kernel of its own because
-// the other copies cost this one registers (1 x 4096 x 4096: 192 us, 217 with both in one).
+// the other copies cost this one registers (1 x 4096 x 4096: 193 us, 217 with both in one).
 template <typename T, int NS, bool EXACT, bool QUICK, int RESIDENT>
 __global__ void __launch_bounds__(32 * kMaxWarps, RESIDENT) scan_kernel(const __grid_constant__ ScanArgs a) {
   using P = Piece<T, NS>;
@@ -338,7 +340,8 @@ int start_pieces(const ScanArgs& a, cudaStream_t s) {
   constexpr int kMost = sizeof(Piece<T, NS>) * kMaxWarps;
   auto kernel = scan_kernel<T, NS, EXACT, QUICK, RESIDENT>;
   if (int e = (int)allow_dynamic_smem<kMost>(kernel)) return e;
-  // as many warps as an average sequence has pieces, two at least: a piece is handed to another warp
+  // as many warps as an average sequence has pieces, two at least: a piece is handed to another warp.  The lengths of packed sequences
+  // are on the device; a long one among many short ones has as few warps as they have.
   const long long longest = a.q.cu ? (a.q.tokens + a.q.count - 1) / a.q.count : a.q.tokens, pieces = (longest + TC - 1) / TC;
   const int warps = pieces > kMaxWarps ? kMaxWarps : pieces < 2 ? 2 : (int)pieces;
   const int per_seq = a.blocks_per_group * (a.channels / a.per_group);
@@ -364,10 +367,13 @@ int start_pieces(const ScanArgs& a, cudaStream_t s) {
 }
 
 // One token for each sequence: the state is read and written once, 8 N bytes a channel, and that is what bounds it (128 sequences x
-// 4096 channels x 16 states 18.5 us, 3.9 TB/s; four sequences of one channel a thread instead 30.5; one of one 34.5).  Four lanes
+// 4096 channels x 16 states 18.8 us, 3.8 TB/s; four sequences of one channel a thread instead 30.5; one of one 37.8).  Four lanes
 // share a channel, four states each at a time (16 bytes).  A thread has R channels of one sequence, a CTA's width apart, so that
 // R loads of states are under way and B and C are read and made float once for them; with R = 4 each lane of the four makes the step
-// size and the output of one of the four channels, and hands the former to the others.
+// size and the output of one of the four channels, and hands the former to the others.  64 registers, so that four CTAs are resident,
+// cost R = 4 some 24 to 48 bytes of spills.
+// R = 4 from kManySteps sequences x channels on: 4 x 4096 of 16 states 2.65 us with R = 1 and 2.97 with R = 4, 8 x 4096 3.6 and 3.05,
+// 16 x 2048 of 64 states 6.7 and 7.9, 32 x 2048 11.5 and 10.8.
 constexpr long long kManySteps = 1 << 15;
 constexpr int kStepThreads = 256, kStepWidth = kStepThreads / 4;
 template <typename T, int R, bool WHOLE>
@@ -477,7 +483,8 @@ int start_step(const ScanArgs& a, cudaStream_t s) {
 template <typename T>
 int start_step(const ScanArgs& a, cudaStream_t s) {
   const bool whole = a.states % 4 == 0 && aligned(a.A, 16) && aligned(a.state, 16);
-  // four channels a thread where that still gives every SM a few CTAs, and where B and C are the same for all of them
+  // four channels a thread where there are many, and where B and C are the same for all of them (in two groups 128 x 4096 take
+  // 37.7 us with one)
   const bool many = a.per_group == a.channels && (long long)a.q.count * a.channels >= kManySteps;
   if (whole) return many ? start_step<T, 4, true>(a, s) : start_step<T, 1, true>(a, s);
   return many ? start_step<T, 4, false>(a, s) : start_step<T, 1, false>(a, s);
